@@ -195,16 +195,13 @@ def work(case):
 # coding (the cache formats), plain
 # ---------------------------------------------------------------------------
 def _code_groups(x, bits, sym, dim):
-    """Codes, scale and offset of groups of 32 along `dim` (which is kept, of length 1).
-    Divisions are by tensors: by a Python number, torch multiplies with its rounded
-    reciprocal on a GPU, which is not the quotient that the formats define."""
+    """Codes, scale and offset of groups of 32 along `dim` (which is kept, of length 1)."""
     if sym:
         top = 2 ** (bits - 1) - 1
-        big = x.abs().amax(dim, keepdim=True)
-        s = (big / torch.full_like(big, top)).clamp_min(1e-8)
+        s = (x.abs().amax(dim, keepdim=True) / top).clamp_min(1e-8)
         return (x / s).round().clamp(-top, top), s.half(), torch.zeros_like(s).half()
     lo, hi = x.amin(dim, keepdim=True), x.amax(dim, keepdim=True)
-    s = ((hi - lo) / torch.full_like(lo, 2 ** bits - 1)).clamp_min(1e-8)
+    s = ((hi - lo) / (2 ** bits - 1)).clamp_min(1e-8)
     return ((x - lo) / s).round().clamp(0, 2 ** bits - 1), s.half(), (lo + 0.0).half()
 
 
@@ -656,14 +653,13 @@ def exact(case, seed):
                 g = done.unflatten(2, (-1, GROUP))                   # [kv, t, groups, 32]
             if case["fmt"] == "sym":
                 top = float(2 ** (case["bits"] - 1) - 1)
-                span = torch.amax(torch.abs(g), -1, True)    # (quotients of tensors, as above)
-                step = torch.clamp(span / torch.full_like(span, top), min=1e-8)
+                step = torch.clamp(torch.amax(torch.abs(g), -1, True) / top, min=1e-8)
                 code = torch.clamp(torch.round(g / step), -top, top)
                 rec = code.double() * step.to(torch.float16).double()
             else:
                 low = torch.amin(g, -1, True)
-                span = torch.amax(g, -1, True) - low
-                step = torch.clamp(span / torch.full_like(span, 2 ** case["bits"] - 1), min=1e-8)
+                step = torch.clamp((torch.amax(g, -1, True) - low) / float(2 ** case["bits"] - 1),
+                                   min=1e-8)
                 code = torch.clamp(torch.round((g - low) / step), 0, 2 ** case["bits"] - 1)
                 rec = (code.double() * step.to(torch.float16).double()
                        + low.to(torch.float16).double())
