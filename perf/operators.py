@@ -552,9 +552,41 @@ def _build_cache(case, x, st):
     for b in range(B):
         last[:, b, :, :new[b]] = x["tail"][:, b, :, tails[b] - new[b]:tails[b]]
     c.append_ragged(last[0], last[1], new)
+    _lay_codes(case, x, c)
     st["cache"] = c
     st["workspace"] = torch.empty(c.attend_shared_workspace(case["rows"]), dtype=torch.uint8,
                                   device=DEV)
+
+
+def _lay_codes(case, x, c):
+    """The cache's codes, scales and offsets as `_pack` gives them, so that both sides attend
+    the same ones.  (On a GPU torch divides by a Python number through its rounded reciprocal,
+    and a few codes in ten thousand, those at ties, differ from the cache's quotients.)"""
+    view, seen, bits = c.planes(), set(), case["bits"]
+    for b in range(case["batch"]):
+        j, t, pages = _branch_of(case, b), _tail(case, b), c.seq_pages(b)
+        first = next((i for i, p in enumerate(pages) if p not in seen), len(pages))
+        seen.update(pages)
+        lo = first * PAGE                                # (the pages before are another's too)
+        hi = _coded(case["fmt"], case["root"] + case["branch"] + t)
+        if lo >= hi:
+            continue
+        for i, n in ((0, "k"), (1, "v")):
+            kv = torch.cat([x["root"][i, 0], x["branch"][i, j], x["tail"][i, b, :, :t]], 1)
+            codes, scale, zero = _pack(case, kv[:, lo:hi], i == 0)
+            codes = codes.reshape(case["kv"], hi - lo, case["dim"]).int()
+            if case["fmt"] == "sym":
+                codes = codes + 2 ** (bits - 1)
+            codes = codes.unflatten(2, (-1, 8 // bits))
+            place = torch.arange(8 // bits, dtype=torch.int32, device=DEV) * bits
+            rows = {n + "_codes": (codes << place).sum(3).to(torch.uint8)}
+            for name, p in ((n + "_scale", scale), (n + "_zero", zero)):
+                if name in view:
+                    rows[name] = p.reshape(case["kv"], -1, view[name].shape[3])
+            for name, r in rows.items():
+                per = _per_page(case, name)
+                at = _index(pages[first:])[:, None] * per + torch.arange(per, device=DEV)
+                view[name][0].index_copy_(1, at.flatten()[:r.shape[1]], r)
 
 
 def _run_attention(st):
