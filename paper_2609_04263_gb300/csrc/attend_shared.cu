@@ -1406,12 +1406,12 @@ leaf_kernel(Geom g, const __nv_bfloat16* __restrict__ q, float scale, LeafSched*
       mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 4));
       mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 8));
       mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], 16));
-      mx[j] = fmaxf(m_run[j], mx[j]);                  // (finite: a block has a token)
+      mx[j] = fmaxf(m_run[j], mx[j]);                  // (-inf: no score above it so far)
     }
     if (__any_sync(0xffffffffu, mx[0] != m_run[0] || mx[1] != m_run[1])) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float alpha = ex2_approx(m_run[j] - mx[j]);
+        const float alpha = m_run[j] == -INFINITY ? 0.f : ex2_approx(m_run[j] - mx[j]);
         m_run[j] = mx[j];
         l_run[j] *= alpha;
 #pragma unroll
@@ -1421,13 +1421,15 @@ leaf_kernel(Geom g, const __nv_bfloat16* __restrict__ q, float scale, LeafSched*
         }
       }
     }
+    // (a head whose scores are all -inf so far, of infinite keys or overflowing products, subtracts 0)
+    const float base[2] = {m_run[0] == -INFINITY ? 0.f : m_run[0], m_run[1] == -INFINITY ? 0.f : m_run[1]};
     uint32_t pb[2][2];
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[i] = ex2_approx(S[mt][i] - m_run[i & 1]);
+        p[i] = ex2_approx(S[mt][i] - base[i & 1]);
         l_run[i & 1] += p[i];
       }
       pb[mt][0] = movmatrix_t(pack_f16(p[0], p[1]));

@@ -1,0 +1,103 @@
+"""Attention over shared pages and by sequence at scores that leave a block, a warp's first
+one or several heads' without a finite maximum, and at values that the format allows and
+random tokens do not reach; against the oracle in fp64."""
+import numpy as np
+import pytest
+import torch
+
+from tests.gpu_common import require_gpu
+from tests.helpers import check_attention, kv_pair
+from tests.test_gpu_pages import Shared
+from tests.test_gpu_shared import _queries, _reference, _replayed
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    require_gpu()
+
+
+class Edited(Shared):
+    """append(n, edit): edit(k, v) changes the new tokens [B, H, L, D] (bf16, on the device)
+    before they are appended."""
+
+    def append(self, n, edit=None):
+        if edit is None:
+            return super().append(n)
+        L = max(max(n), 1)
+        k, v, _, _ = kv_pair(self.B, self.H, L, self.D, "bf16", seed=self.seed, stream=self.step)
+        self.step += 1
+        edit(k, v)
+        self.gc.append_ragged(k, v, n)
+        nk, nv = k.float().cpu().numpy(), v.float().cpu().numpy()
+        for b in range(self.B):
+            if n[b]:
+                new = (nk[b:b + 1, :, :n[b]], nv[b:b + 1, :, :n[b]])
+                self.oc[b].append(*new)
+                self.hist[b] = tuple(np.concatenate([h, x], 2) for h, x in zip(self.hist[b], new))
+        self.n_last = list(n)
+        return L
+
+
+def _decodes(bt, qd):
+    return {"shared": bt.gc.attend_decode_shared(qd),
+            "shared, captured": _replayed(bt.gc.attend_decode_shared, qd, bt.gc.attend_shared_workspace())}
+
+
+def _prefills(bt, qd, L):
+    return {"shared": bt.gc.attend_prefill_shared(qd),
+            "shared, captured": _replayed(bt.gc.attend_prefill_shared, qd, bt.gc.attend_shared_workspace(L))}
+
+
+def _check(bt, outs, q, rows=None):
+    for name, out in outs.items():
+        out = out.float().cpu().numpy()
+        for b in range(bt.B):
+            n = q.shape[2] if rows is None else rows[b]
+            if n and bt.oc[b].T:
+                with np.errstate(invalid="ignore", over="ignore"):
+                    ref = _reference(bt, b, q[b:b + 1, :, :n])
+                check_attention(out[b:b + 1, :, :n], ref, "bf16", f"{name}, sequence {b}")
+
+
+@pytest.mark.parametrize("H,Hq,D", [(2, 8, 128), (1, 16, 64), (2, 2, 64)])
+@pytest.mark.parametrize("shared", [0, 600])
+def test_blocks_whose_scores_are_all_minus_infinity(H, Hq, D, shared):
+    """Keys of -inf in a channel where the query is 1: tokens without weight, here most of a
+    KIVI window, whole blocks of it among them, and the window's first or last block alone."""
+    bt = Edited("kivi2", 4, H, Hq, D, 1400, num_pages=30, seed=D + shared)
+    if shared:
+        bt.append([shared, 0, 0, 0])
+        bt.fork([0, 0, 0], [1, 2, 3])
+
+    def edit(k, v):
+        k[0, :, 1:, 3] = float("-inf")       # all but one token
+        k[1, :, -33:, 3] = float("-inf")     # the last block, and what is before it in part
+        k[2, :, :70, 3] = float("-inf")      # the first blocks
+        k[3, :, ::2, 3] = float("-inf")
+    # (below the window's 128 tokens: an infinite key is never coded)
+    L = bt.append([97, 97, 97, 65], edit)
+    q = _queries(bt, 1, 3)
+    q[..., 3] = 1.0
+    _check(bt, _decodes(bt, q.cuda()), q)
+    q = _queries(bt, L, 4)
+    q[..., 3] = 1.0
+    if shared:                               # (without: rows of sequence 2 that see no finite score)
+        _check(bt, _prefills(bt, q.cuda(), L), q, bt.n_last)
+
+
+def test_scores_that_overflow_for_one_head_of_two():
+    """Keys of 2^127 in a channel: -inf for a head whose query there is -2^10, finite for its
+    neighbour's 2^-120."""
+    bt = Edited("kivi4", 3, 1, 4, 64, 900, num_pages=12, seed=8)
+
+    def edit(k, v):
+        k[0, :, :64, 5] = 2.0 ** 127
+        k[1, :, -40:, 5] = 2.0 ** 127
+        k[2, :, 31:64, 5] = 2.0 ** 127
+    bt.append([100, 97, 65], edit)
+    q = _queries(bt, 1, 5)
+    q[:, 0::2, :, 5] = -2.0 ** 10
+    q[:, 1::2, :, 5] = 2.0 ** -120
+    _check(bt, _decodes(bt, q.cuda()), q)
