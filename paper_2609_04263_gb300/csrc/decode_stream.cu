@@ -677,13 +677,15 @@ decode_stream_kernel(Geom g, const __nv_bfloat16* __restrict__ q, float scale, i
       offa[0] *= alpha[0]; offa[1] *= alpha[1];
       offa[2] *= alpha[0]; offa[3] *= alpha[1];
     }
+    // (a head whose scores are all -inf so far, of infinite keys or overflowing products, subtracts 0)
+    const float base[2] = {m_run[0] == -INFINITY ? 0.f : m_run[0], m_run[1] == -INFINITY ? 0.f : m_run[1]};
     uint32_t pb[2][2];                               // B fragments of P^T per 16-token step
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[i] = exp2f(S[mt][i] - m_run[i & 1]);       // exp2(-inf) = 0
+        p[i] = exp2f(S[mt][i] - base[i & 1]);        // exp2(-inf) = 0
         l_run[i & 1] += p[i];
       }
       pb[mt][0] = movmatrix_t(pack_f16(p[0], p[1]));

@@ -58,6 +58,7 @@ def _check(bt, outs, q, rows=None):
             if n and bt.oc[b].T:
                 with np.errstate(invalid="ignore", over="ignore"):
                     ref = _reference(bt, b, q[b:b + 1, :, :n])
+                assert np.isfinite(ref).all()
                 check_attention(out[b:b + 1, :, :n], ref, "bf16", f"{name}, sequence {b}")
 
 
@@ -90,7 +91,7 @@ def test_blocks_whose_scores_are_all_minus_infinity(H, Hq, D, shared):
 def test_scores_that_overflow_for_one_head_of_two():
     """Keys of 2^127 in a channel: -inf for a head whose query there is -2^10, finite for its
     neighbour's 2^-120."""
-    bt = Edited("kivi4", 3, 1, 4, 64, 900, num_pages=12, seed=8)
+    bt = Edited("kivi2", 3, 1, 4, 64, 900, num_pages=12, seed=8)
 
     def edit(k, v):
         k[0, :, :64, 5] = 2.0 ** 127
@@ -101,3 +102,23 @@ def test_scores_that_overflow_for_one_head_of_two():
     q[:, 0::2, :, 5] = -2.0 ** 10
     q[:, 1::2, :, 5] = 2.0 ** -120
     _check(bt, _decodes(bt, q.cuda()), q)
+
+
+@pytest.mark.parametrize("fmt", ["kivi2", "kivi4"])
+def test_minus_infinity_by_sequence(fmt):
+    """The same windows through attend_decode of a cache long enough for its streaming kernel (16
+    32-token blocks a SM): each of its warps takes a block in turn, so most begin with such a one."""
+    bt = Edited(fmt, 10, 8, 16, 64, 1200, num_pages=60, seed=41)
+    bt.append([1000] * 10)
+
+    def edit(k, v):
+        k[:, :, :, 3] = float("-inf")
+        k[1, :, -1, 3] = 0.5
+    bt.append([60] * 10, edit)               # (a kivi4 cache's window keeps 64)
+    q = _queries(bt, 1, 3)
+    q[..., 3] = 1.0
+    out = bt.gc.attend_decode(q.cuda()).float().cpu().numpy()
+    for b in (0, 1, 9):
+        ref = _reference(bt, b, q[b:b + 1])
+        assert np.isfinite(ref).all()
+        check_attention(out[b:b + 1], ref, "bf16", f"sequence {b}")
