@@ -328,17 +328,16 @@ attend_prefill_m256_kernel(Geom g, const __nv_bfloat16* __restrict__ q, int L, f
       }
       // P = 2^(s c2 - m) as fp16 pairs over the first 32 columns of this S
       // buffer (masked keys hold -inf: 2^-inf = 0; a row without any visible
-      // key so far has m = -inf and keeps P = 0)
-      const bool live = m != -INFINITY;
-      const uint64_t negm = f2pack(-m, -m);
+      // key so far has m = -inf and subtracts 0; a NaN score is a NaN P)
+      const float nm = m == -INFINITY ? 0.f : -m;
+      const uint64_t negm = f2pack(nm, nm);
       uint64_t sum2 = f2pack(0.f, 0.f);
       uint32_t pk[kTok / 2];
 #pragma unroll
       for (int i = 0; i < kTok; i += 2) {
         float a0, a1;
         f2unpack(ffma2(f2pack(__uint_as_float(sr[i]), __uint_as_float(sr[i + 1])), c22, negm), a0, a1);
-        float p0 = ex2_approx(a0), p1 = ex2_approx(a1);
-        if (!live) p0 = p1 = 0.f;
+        const float p0 = ex2_approx(a0), p1 = ex2_approx(a1);
         sum2 = fadd2(sum2, f2pack(p0, p1));
         pk[i / 2] = pack_h2(p0, p1);
       }
@@ -358,7 +357,7 @@ attend_prefill_m256_kernel(Geom g, const __nv_bfloat16* __restrict__ q, int L, f
       ok = false;
     if (__all_sync(0xffffffffu, ok && !*abort)) {
       tc_fence_after();
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const float inv = l == 0.f ? 0.f : 1.f / l;        // (no visible key: 0; NaN stays)
       const int hl = row / nq, qi = row % nq;
       __nv_bfloat16* dst = out + (((int64_t)b * g.Hq + hkv * grp + hl) * L + q0 + qi) * D;
 #pragma unroll 1

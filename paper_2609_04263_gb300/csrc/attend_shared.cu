@@ -1625,7 +1625,8 @@ merge_kernel(const __grid_constant__ Geom g, int L, int decode, const SchedOut* 
               8 * D + 2 * (hl & 7));
       }
     }
-    const float2 ml = mlp ? *reinterpret_cast<const float2*>(mlp) : make_float2(-INFINITY, 0.f);
+    float2 ml = mlp ? *reinterpret_cast<const float2*>(mlp) : make_float2(-INFINITY, 0.f);
+    if (ml.y != ml.y) ml.x = INFINITY;                   // a NaN score (maxima skip it): the row is NaN
     float mb = ml.x;
 #pragma unroll
     for (int k = 16; k; k >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, k));
@@ -1679,7 +1680,7 @@ merge_kernel(const __grid_constant__ Geom g, int L, int decode, const SchedOut* 
       for (int v = 0; v < V; ++v) acc[v] = fmaf(fk, wo[warp + k][V * lane + v], acc[v]);
     }
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;        // (no visible key: 0)
   uint32_t pk[V / 2];
 #pragma unroll
   for (int v = 0; v < V; v += 2) pk[v / 2] = pack_bf16(acc[v] * inv, acc[v + 1] * inv);

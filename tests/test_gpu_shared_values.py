@@ -122,3 +122,37 @@ def test_minus_infinity_by_sequence(fmt):
         ref = _reference(bt, b, q[b:b + 1])
         assert np.isfinite(ref).all()
         check_attention(out[b:b + 1], ref, "bf16", f"sequence {b}")
+
+
+@pytest.mark.parametrize("fmt,H,Hq,D", [("kivi2", 2, 8, 128), ("affine4", 2, 8, 64), ("sym2", 1, 4, 128)])
+def test_nan_stays_in_its_row(fmt, H, Hq, D):
+    """A NaN query (all of it, or one channel) makes its own row NaN and no other; eagerly and
+    captured, prompts short and long enough to go sequence by sequence."""
+    bt = Edited(fmt, 4, H, Hq, D, 1600, num_pages=30, seed=2)
+    bt.append([600, 0, 0, 0])
+    bt.fork([0, 0], [1, 2])
+    for n in ([1, 40, 3, 70], [5, 700, 300, 600]):
+        L = bt.append(n)
+        q = _queries(bt, 1, 6)
+        q[0, 1], q[1, 0, 0, 7], q[3, -1] = float("nan"), float("nan"), float("nan")
+        bad = np.zeros((bt.B, Hq), bool)
+        bad[0, 1] = bad[1, 0] = bad[3, -1] = True
+        for name, out in _decodes(bt, q.cuda()).items():
+            out = out.float().cpu().numpy()
+            for b in range(bt.B):
+                assert np.isnan(out[b, bad[b]]).all(), name
+                ref = _reference(bt, b, torch.nan_to_num(q[b:b + 1]))
+                check_attention(out[b:b + 1, ~bad[b]], ref[:, ~bad[b]], "bf16", name)
+        q = _queries(bt, L, 6)
+        bad = np.zeros((bt.B, Hq, L), bool)
+        for b, h, l in ((0, 1, 0), (1, 0, n[1] - 1), (1, 0, 17), (3, Hq - 1, 64)):
+            if l < n[b]:
+                q[b, h, l] = float("nan")
+                bad[b, h, l] = True
+        for name, out in _prefills(bt, q.cuda(), L).items():
+            out = out.float().cpu().numpy()
+            for b in range(bt.B):
+                w, o = bad[b, :, :n[b]], out[b, :, :n[b]]
+                assert np.isnan(o[w]).all(), name
+                ref = _reference(bt, b, torch.nan_to_num(q[b:b + 1, :, :n[b]]))[0]
+                check_attention(o[~w], ref[~w], "bf16", name)
