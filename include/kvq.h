@@ -439,8 +439,8 @@ int kvq_seq_tokens(const kvq_cache* cache, int b);
 
 /* Layouts RAGGED and PAGED: sequence b becomes empty (T_b = 0) and a PAGED
  * cache returns its pages to the pool (those that no other sequence shares).
- * Stream-ordered like an append; not captured once a cache has had forks
- * (KVQ_ERR_UNSUPPORTED). */
+ * Stream-ordered like an append; a PAGED cache's release cannot be captured in a
+ * graph (KVQ_ERR_UNSUPPORTED): its pages change hands on the host. */
 kvq_status kvq_seq_release(kvq_cache* cache, int b, void* stream);
 
 /* Pages of a PAGED cache's pool not held by any sequence (-1 otherwise). */

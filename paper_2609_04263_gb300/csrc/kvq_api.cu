@@ -511,12 +511,13 @@ kvq_status kvq_seq_release(kvq_cache* cache, int b, void* stream) {
   if (b < 0 || b >= cache->g.B) return fail(KVQ_ERR_ARG, "sequence %d outside [0, %d)", b, cache->g.B);
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
-  if (!cache->plan.empty()) {
-    // a replay would send the shared runs of now again
+  if (cache->g.layout == KVQ_LAYOUT_PAGED) {
+    // the pages go back on the host once, now; a replay would empty the sequence on the device
+    // alone, whose pages others may have come to share since
     cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
     e = cudaStreamIsCapturing(s, &st);
     if (e == cudaSuccess && st != cudaStreamCaptureStatusNone)
-      return fail(KVQ_ERR_UNSUPPORTED, "kvq_seq_release of a cache with forks cannot be captured in a graph");
+      return fail(KVQ_ERR_UNSUPPORTED, "kvq_seq_release of a paged cache cannot be captured in a graph");
   }
   if (e == cudaSuccess) e = ensure_init(cache, s);
   if (e == cudaSuccess) e = launch_seq_reset(cache->g, b, s);
