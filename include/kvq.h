@@ -174,8 +174,8 @@ int kvq_cache_tokens(const kvq_cache* cache);
 
 /* Read the device token count into the host mirror (synchronises `stream`).
  * Returns KVQ_ERR_CAPACITY (and clears the flag) if a replayed append was
- * refused on the device because it would exceed max_tokens; a refused
- * append writes nothing and leaves T unchanged. */
+ * refused on the device because it would exceed max_tokens (or, PAGED, the pages
+ * that a sequence holds); a refused append writes nothing and leaves T unchanged. */
 kvq_status kvq_cache_sync(kvq_cache* cache, void* stream);
 
 /* Device pointers and shapes of every plane (for tests and export). */
@@ -426,10 +426,13 @@ kvq_status kvq_lora_backward(const void* x, int B, int L, int d_in, const void* 
  * kvq_attend_decode then attend, per sequence, the n[b] rows of the last
  * append (prefill: rows l < n[b] of q and out; the rest of out is not
  * written) or its newest token (decode; a sequence holding no token gets a
- * zero output) over that sequence's T_b tokens.  A PAGED append that takes
- * new pages copies their table entries from host memory on `stream`, so it
- * must not be captured in a CUDA graph; RAGGED appends and the attention
- * calls can be (kvq_cache_sync then refreshes the host's per-sequence counts).
+ * zero output) over that sequence's T_b tokens.  RAGGED appends and the
+ * attention calls can be captured in a CUDA graph (kvq_cache_sync then
+ * refreshes the host's per-sequence counts), and PAGED appends that take no new
+ * page (otherwise KVQ_ERR_UNSUPPORTED).  Pages are taken on the host alone: a
+ * replay by which some sequence would pass max_tokens, or, PAGED, the
+ * last page of its present tokens, appends nothing to any sequence (n[b] = 0) and
+ * sets the cache's error bit (kvq_cache_sync: KVQ_ERR_CAPACITY).
  */
 kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v, int L,
                                   const int* n, void* stream);

@@ -471,7 +471,17 @@ kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v
     return fail(KVQ_ERR_CAPACITY, "the append needs %d pages, %d are free", need_pages,
                 cache->n_free);
   cudaStream_t s = (cudaStream_t)stream;
-  cudaError_t e = ensure_init(cache, s);
+  cudaError_t e = cudaSuccess;
+  bool captured = false;
+  if (g.layout == KVQ_LAYOUT_PAGED) {
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    e = cudaStreamIsCapturing(s, &st);
+    captured = st != cudaStreamCaptureStatusNone;
+    if (e == cudaSuccess && captured && need_pages > 0)
+      return fail(KVQ_ERR_UNSUPPORTED, "an append that takes new pages (%d) cannot be captured in a graph",
+                  need_pages);
+  }
+  if (e == cudaSuccess) e = ensure_init(cache, s);
   if (e != cudaSuccess) return cuda_fail(e, "kvq_append_pack_ragged");
   if (g.layout == KVQ_LAYOUT_PAGED) {
     for (int b = 0; b < g.B; ++b) {
@@ -487,7 +497,11 @@ kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v
       if (e != cudaSuccess) return cuda_fail(e, "kvq_append_pack_ragged page table");
     }
   }
-  e = launch_append_ragged(g, L, k, v, cnt.data(), s);
+  std::vector<int> room(g.B, g.Tmax);
+  if (g.layout == KVQ_LAYOUT_PAGED)
+    for (int b = 0; b < g.B; ++b)
+      room[b] = captured ? -1 : (int)std::min<int64_t>(g.Tmax, (int64_t)cache->seq_pages[b].size() * kPageTok);
+  e = launch_append_ragged(g, L, k, v, cnt.data(), room.data(), s);
   if (e != cudaSuccess) return cuda_fail(e, "kvq_append_pack_ragged launch");
   int tmax = 0;
   for (int b = 0; b < g.B; ++b) {

@@ -162,9 +162,11 @@ cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t sme
 // All launchers read the token count from g.state on the device.
 cudaError_t launch_append(const Geom& g, int L, const void* k, const void* v, cudaStream_t s);
 // RAGGED / PAGED: sequence b appends its first n[b] (host array) of L tokens;
-// then its device count advances.  seq_reset: sequence b becomes empty.
+// then its device count advances.  room[b] (host array): tokens that it may come to hold, or
+// -1 for those that the pages of its count on the device hold.  seq_reset: sequence b
+// becomes empty.
 cudaError_t launch_append_ragged(const Geom& g, int L, const void* k, const void* v,
-                                 const int* n, cudaStream_t s);
+                                 const int* n, const int* room, cudaStream_t s);
 cudaError_t launch_seq_reset(const Geom& g, int b, cudaStream_t s);
 // t_hint: the host's count of stored tokens, used only to choose between
 // decode kernels (the kernels read the count from the device).

@@ -4,6 +4,8 @@
 // format fixes, so codes and fp16 metadata are reproducible bit for bit.
 #include <math.h>
 
+#include <algorithm>
+
 #include "kvq_internal.cuh"
 #include "quant_common.cuh"
 
@@ -148,15 +150,26 @@ __global__ void pack_pertoken_kernel(Geom g, int L, TokSrc sk, TokSrc sv, int sy
 }
 
 // Ragged appends: this append's counts (first), and the sequences' counts
-// advanced by them (last).
+// advanced by them (last).  Sequence b may come to hold room[b] tokens (-1, a captured
+// append to a PAGED cache: what the pages of its present count hold, since a replay takes
+// none).  An append of which some sequence would hold more is refused whole.
 struct SeqCounts {
-  int32_t n[KVQ_MAX_SEQS];
+  int32_t n[KVQ_MAX_SEQS], room[KVQ_MAX_SEQS];
 };
 
-__global__ void seq_counts_kernel(Geom g, SeqCounts n) {
+__global__ void seq_counts_kernel(Geom g, const __grid_constant__ SeqCounts c) {
   pdl_wait();
   pdl_trigger();
-  for (int b = threadIdx.x; b < g.B; b += blockDim.x) g.seq_new[b] = n.n[b];
+  bool fits = true;
+  for (int b = threadIdx.x; b < g.B; b += blockDim.x) {
+    const int T = g.seq_len[b], n = c.n[b];
+    const int64_t room = c.room[b] >= 0 ? c.room[b]
+                                        : min((int64_t)g.Tmax, ((int64_t)T + kPageTok - 1) / kPageTok * kPageTok);
+    fits = fits && (n == 0 || (int64_t)T + n <= room);
+  }
+  fits = __syncthreads_and(fits);
+  for (int b = threadIdx.x; b < g.B; b += blockDim.x) g.seq_new[b] = fits ? c.n[b] : 0;
+  if (!fits && threadIdx.x == 0) atomicOr(&g.state->error, kErrCapacity);
 }
 
 __global__ void seq_advance_kernel(Geom g) {
@@ -1120,9 +1133,10 @@ cudaError_t launch_kivi_append(const Geom& g, int L, const void* k, const void* 
 }  // namespace
 
 cudaError_t launch_append_ragged(const Geom& g, int L, const void* k, const void* v,
-                                 const int* n, cudaStream_t s) {
+                                 const int* n, const int* room, cudaStream_t s) {
   SeqCounts c = {};
-  for (int b = 0; b < g.B; ++b) c.n[b] = n[b];
+  std::copy(n, n + g.B, c.n);
+  std::copy(room, room + g.B, c.room);
   launch_pdl(seq_counts_kernel, dim3(1), dim3(256), 0, s, g, c);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
