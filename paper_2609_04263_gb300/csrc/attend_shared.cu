@@ -1873,6 +1873,18 @@ static kvq_status attend_shared(kvq_cache* cache, const void* q, int L, int n_q_
     return set_error(KVQ_ERR_ARG, "workspace must be 256-byte aligned");
   if (!countable(g, L))
     return set_error(KVQ_ERR_SHAPE, "%d query rows a sequence are too many for one call", L);
+  cudaStream_t s = (cudaStream_t)stream;
+  cudaError_t e = cudaSuccess;
+  if (!cache->plan_known) {
+    // a launch failed since the plan was last sent: all of it goes first
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    e = cudaStreamIsCapturing(s, &st);
+    if (e == cudaSuccess && st != cudaStreamCaptureStatusNone)
+      return set_error(KVQ_ERR_UNSUPPORTED, "the shared pages are sent anew after a failed launch: this "
+                       "call cannot be captured in a graph");
+    if (e == cudaSuccess) e = update_shared_plan(cache, s);
+    if (e != cudaSuccess) return set_error(KVQ_ERR_CUDA, "attend_shared: %s", cudaGetErrorString(e));
+  }
   const size_t need = kvq_attend_shared_workspace(cache, L);
   if (workspace_bytes < need)
     return set_error(KVQ_ERR_CAPACITY, "workspace of %zu bytes < %zu", workspace_bytes, need);
@@ -1890,8 +1902,6 @@ static kvq_status attend_shared(kvq_cache* cache, const void* q, int L, int n_q_
   c.leaf = reinterpret_cast<float*>(static_cast<char*>(workspace) + leaf_at());
   c.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + slots_at(g));
   c.cap = (int)std::min<size_t>((workspace_bytes - slots_at(g)) / (slot_floats(g.D) * 4), 1 << 30);
-  cudaStream_t s = (cudaStream_t)stream;
-  cudaError_t e = cudaSuccess;
   // (captured calls always run the kernels here: a replay follows the forks and lengths of its
   // time)
   if (!decode && alone_faster(cache)) {

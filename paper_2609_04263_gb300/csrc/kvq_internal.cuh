@@ -437,6 +437,7 @@ struct kvq_cache {
   int n_free = 0, free_from = 0;    // free pages; no word of free_bits below this has one
   std::vector<int> page_refs;       // sequences that hold each page
   std::vector<int32_t> plan;        // the plan words last sent to the device (empty: zeros)
+  bool plan_known = true;           // false: a launch failed, the device may hold other words
 };
 
 namespace kvq {
@@ -448,7 +449,8 @@ cudaError_t ensure_cache_init(kvq_cache* c, cudaStream_t s);
 int page_take(kvq_cache* c);
 void page_drop(kvq_cache* c, int page);
 void pages_reset(kvq_cache* c);      // every page free, nothing shared
-// Rebuild the plan of shared pages and send it, where it differs from the device's.
+// Rebuild the plan of shared pages and send it, where it differs from the device's (or all
+// of it, where that is not known).
 cudaError_t update_shared_plan(kvq_cache* c, cudaStream_t s);
 // Largest count over the sequences, after one of them changed.
 void refresh_max_tokens(kvq_cache* c);

@@ -58,6 +58,7 @@ void pages_reset(kvq_cache* c) {
   c->page_refs.assign(n, 0);
   free_above(c, 0);
   c->plan.clear();                                       // the device's is zeroed with its state
+  c->plan_known = true;
 }
 
 void refresh_max_tokens(kvq_cache* c) {
@@ -368,12 +369,12 @@ struct PlanBuilder {
 };
 
 template <int N>
-void launch_words_n(const Geom& g, const int32_t* w, int at, int n, cudaStream_t s) {
+cudaError_t launch_words_n(const Geom& g, const int32_t* w, int at, int n, cudaStream_t s) {
   Words<N> a;
   a.n = n;
   a.at = at;
   std::copy(w + at, w + at + n, a.w);
-  launch_pdl(plan_words_kernel<N>, dim3(1), dim3(256), 0, s, g, a);
+  return launch_pdl(plan_words_kernel<N>, dim3(1), dim3(256), 0, s, g, a);
 }
 
 }  // namespace
@@ -384,7 +385,7 @@ static cudaError_t send_shared_plan(kvq_cache* c, cudaStream_t s) {
   bool shared = false;
   for (int b = 0; b < g.B && !shared; ++b)
     shared = !c->seq_pages[b].empty() && c->page_refs[c->seq_pages[b][0]] > 1;
-  if (!shared && c->plan.empty()) return cudaSuccess;    // none before, none now
+  if (!shared && c->plan.empty() && c->plan_known) return cudaSuccess;   // none before, none now
   PlanBuilder pb{c, {}, {}, std::vector<int32_t>(g.B, 0), std::vector<int32_t>(g.B, 0)};
   std::vector<int> all(g.B);
   for (int b = 0; b < g.B; ++b) all[b] = b;
@@ -400,18 +401,21 @@ static cudaError_t send_shared_plan(kvq_cache* c, cudaStream_t s) {
   std::copy(pb.leaf_parent.begin(), pb.leaf_parent.end(), w.begin() + kPlanNodes + 2 * g.B);
   // the changed range alone, in argument-sized pieces
   int lo = 0, hi = (int)w.size();
-  if (c->plan.size() == w.size()) {
+  if (c->plan_known && c->plan.size() == w.size()) {
     while (lo < hi && w[lo] == c->plan[lo]) ++lo;
     while (hi > lo && w[hi - 1] == c->plan[hi - 1]) --hi;
   }
   c->plan.swap(w);
+  c->plan_known = false;
   constexpr int N = 4000, n = 700;
-  for (int at = lo; at < hi; at += N) {
+  cudaError_t e = cudaSuccess;
+  for (int at = lo; at < hi && e == cudaSuccess; at += N) {
     const int k = std::min(N, hi - at);
-    if (k <= n) launch_words_n<n>(g, c->plan.data(), at, k, s);
-    else launch_words_n<N>(g, c->plan.data(), at, k, s);
+    e = k <= n ? launch_words_n<n>(g, c->plan.data(), at, k, s) : launch_words_n<N>(g, c->plan.data(), at, k, s);
   }
-  return cudaGetLastError();
+  c->plan_known = e == cudaSuccess;
+  if (e != cudaSuccess) (void)cudaGetLastError();        // (reported here)
+  return e;
 }
 
 cudaError_t update_shared_plan(kvq_cache* c, cudaStream_t s) {
@@ -421,7 +425,9 @@ cudaError_t update_shared_plan(kvq_cache* c, cudaStream_t s) {
   } catch (...) {
     // the plan without shared runs is right for any pages, and needs no memory
     c->plan.clear();
-    return cudaMemsetAsync(c->g.shared_plan, 0, (size_t)plan_words(c->g.B) * 4, s);
+    const cudaError_t e = cudaMemsetAsync(c->g.shared_plan, 0, (size_t)plan_words(c->g.B) * 4, s);
+    c->plan_known = e == cudaSuccess;
+    return e;
   }
 }
 
@@ -562,7 +568,8 @@ kvq_status take_sequences(const char* what, kvq_cache* to, kvq_cache* from, int 
   }
   refresh_max_tokens(to);
   e = launch_takes(g, from->g, takes, fresh, window, s);
-  if (e == cudaSuccess) e = update_shared_plan(to, s);
+  const cudaError_t sent = update_shared_plan(to, s);    // (of the lists as they are, whatever e is)
+  if (e == cudaSuccess) e = sent;
   return e == cudaSuccess ? KVQ_OK : cuda_error(e, what);
 }
 
@@ -641,7 +648,8 @@ kvq_status truncate(kvq_cache* c, int n, const int* seqs, const int* tokens, cud
   }
   refresh_max_tokens(c);
   e = launch_changes(g, edits, entries, jobs, s);
-  if (e == cudaSuccess) e = update_shared_plan(c, s);
+  const cudaError_t sent = update_shared_plan(c, s);
+  if (e == cudaSuccess) e = sent;
   return e == cudaSuccess ? KVQ_OK : cuda_error(e, what);
 }
 

@@ -1,5 +1,7 @@
 """Captured calls on ragged and paged caches: what is refused, what a replay may do to a cache that
 has been forked, cut and compacted since, and what the host finds after kvq_cache_sync."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -14,6 +16,15 @@ pytestmark = pytest.mark.gpu
 @pytest.fixture(scope="module", autouse=True)
 def _gpu():
     require_gpu()
+
+
+@pytest.fixture(autouse=True)
+def _no_graph_left():
+    """A graph that a caught exception's frames still hold is freed here: freed in the middle of
+    another capture, it would end that one."""
+    gc.collect()
+    yield
+    gc.collect()
 
 
 def _refused_in_capture(call, status=kvq.KVQ_ERR_UNSUPPORTED):

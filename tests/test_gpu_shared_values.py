@@ -1,6 +1,8 @@
 """Attention over shared pages and by sequence at scores that leave a block, a warp's first
 one or several heads' without a finite maximum, and at values that the format allows and
 random tokens do not reach; against the oracle in fp64."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -16,6 +18,15 @@ pytestmark = pytest.mark.gpu
 @pytest.fixture(scope="module", autouse=True)
 def _gpu():
     require_gpu()
+
+
+@pytest.fixture(autouse=True)
+def _no_graph_left():
+    """A graph that a caught exception's frames still hold is freed here: freed in the middle of
+    another capture, it would end that one."""
+    gc.collect()
+    yield
+    gc.collect()
 
 
 class Edited(Shared):
