@@ -1282,19 +1282,21 @@ leaf_kernel(Geom g, const __nv_bfloat16* __restrict__ q, float scale, LeafSched*
         for (int mt = 0; mt < 2; ++mt) S[mt][0] = S[mt][1] = S[mt][2] = S[mt][3] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KSS; ++ks) {
-          uint32_t bh[2], bl[2], az[2];
+          uint32_t bh[2], bl[2], az[2], bz[2];
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
             const int i = 2 * ks + hf;
             const int sel = (Z::lo(i) & 1) ? 0x7632 : 0x5410;
             const uint32_t as = __byte_perm(sw[Z::lo(i) >> 1], sw[Z::hi(i) >> 1], sel);
             const uint32_t w2 = ((uint32_t)(15 + Z::e(i % Z::RPW)) << 10) * 0x00010001u;   // (2^e, 2^e)
-            az[hf] = hmul2u(__byte_perm(zw[Z::lo(i) >> 1], zw[Z::hi(i) >> 1], sel), w2);
+            // (q taken back up by 2^e, exactly, and not z, which would overflow from 2^12 on)
+            az[hf] = __byte_perm(zw[Z::lo(i) >> 1], zw[Z::hi(i) >> 1], sel);
+            bz[hf] = hmul2u(qw[i], w2);
             bh[hf] = hmul2u(qw[i], as);
             bl[hf] = hfma2u_neg(qw[i], as, bh[hf]);
           }
           const uint32_t aZ[4] = {az[0], az[0], az[1], az[1]};
-          mma16816_f16(sz, aZ, qw[2 * ks], qw[2 * ks + 1]);
+          mma16816_f16(sz, aZ, bz[0], bz[1]);
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt) {
             uint32_t a[4];

@@ -167,3 +167,28 @@ def test_nan_stays_in_its_row(fmt, H, Hq, D):
                 assert np.isnan(o[w]).all(), name
                 ref = _reference(bt, b, torch.nan_to_num(q[b:b + 1, :, :n[b]]))[0]
                 check_attention(o[~w], ref[~w], "bf16", name)
+
+
+@pytest.mark.parametrize("fmt", ["kivi2", "kivi4"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_offsets(fmt, D):
+    """A key channel of +-10,000 to 40,000 with steps of its range, against queries of 2^-13 there:
+    offsets of all fp16's range, in the own tokens and in the shared ones."""
+    bt = Edited(fmt, 4, 2, 8, D, 1200, num_pages=24, seed=D)
+
+    def edit(k, v):
+        k[:, 0, :, 7] = 100 * k[:, 0, :, 7] + 30000
+        k[:, 1, :, D - 9] = 100 * k[:, 1, :, D - 9] - 10000
+        k[:, 1, :, 2] = 40000
+    bt.append([0, 0, 700, 300], edit)
+    bt.append([600, 1, 33, 300], edit)
+    bt.fork([0], [1])
+    L = bt.append([40, 90, 1, 160], edit)
+    for n in (1, L):
+        q = _queries(bt, n, 9)
+        for h, c in ((0, 7), (1, D - 9), (1, 2)):
+            q[:, 4 * h:4 * h + 4, :, c] = 2.0 ** -13 * torch.sign(q[:, 4 * h:4 * h + 4, :, c])
+        if n == 1:
+            _check(bt, _decodes(bt, q.cuda()), q)
+        else:
+            _check(bt, _prefills(bt, q.cuda(), L), q, bt.n_last)
