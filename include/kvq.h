@@ -158,7 +158,10 @@ size_t kvq_cache_bytes(const kvq_cache_desc* desc);
  * The token count T lives in device memory and kernels read it there, so a
  * sequence of calls can be captured into a CUDA graph and replayed: every
  * replayed append advances T on the device.  The host keeps a mirror for
- * argument checks; after replays, kvq_cache_sync() refreshes it. */
+ * argument checks; after replays, kvq_cache_sync() refreshes it.  (The first
+ * launching call after create or reset is captured with its zeroing, which
+ * replays repeat; on a PAGED cache it is refused in a capture,
+ * KVQ_ERR_UNSUPPORTED.) */
 kvq_status kvq_create_cache(const kvq_cache_desc* desc, void* dev_buf, size_t bytes,
                             kvq_cache** out);
 

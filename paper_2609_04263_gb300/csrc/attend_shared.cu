@@ -1914,6 +1914,9 @@ static kvq_status attend_shared(kvq_cache* cache, const void* q, int L, int n_q_
   }
   if (e == cudaSuccess) e = ensure_cache_init(cache, s);
   if (e == cudaSuccess) e = launch_shared(g, c, s);
+  if (e == cudaErrorStreamCaptureUnsupported)
+    return set_error(KVQ_ERR_UNSUPPORTED, "attend_shared: the first call on a paged cache after it was created "
+                     "or reset cannot be captured in a graph: its replays would empty the cache");
   if (e != cudaSuccess) return set_error(KVQ_ERR_CUDA, "attend_shared: %s", cudaGetErrorString(e));
   return KVQ_OK;
 }

@@ -32,6 +32,9 @@ kvq_status fail(kvq_status st, const char* fmt, ...) {
 }
 
 kvq_status cuda_fail(cudaError_t e, const char* where) {
+  if (e == cudaErrorStreamCaptureUnsupported)            // (ensure_cache_init)
+    return fail(KVQ_ERR_UNSUPPORTED, "%s: the first call on a paged cache after it was created or reset "
+                "cannot be captured in a graph: its replays would empty the cache", where);
   return fail(KVQ_ERR_CUDA, "%s: %s", where, cudaGetErrorString(e));
 }
 
@@ -236,10 +239,17 @@ int* device_error_word() {
 }
 
 // Zero the device state before the first launch after create/reset
-// (stream-ordered, so it can be captured with the calls that follow).
+// (stream-ordered, so it can be captured with the calls that follow; not for a PAGED cache,
+// whose lists on the host would not follow a replay that empties it).
 cudaError_t ensure_cache_init(kvq_cache* c, cudaStream_t s) {
   if (!c->need_init) return cudaSuccess;
   cudaError_t e = cudaSuccess;
+  if (c->g.layout == KVQ_LAYOUT_PAGED) {
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    e = cudaStreamIsCapturing(s, &st);
+    if (e == cudaSuccess && st != cudaStreamCaptureStatusNone) e = cudaErrorStreamCaptureUnsupported;
+    if (e != cudaSuccess) return e;
+  }
   if (c->need_clear) {
     // once per buffer: the workspace (whose tagged words the fused decode
     // step matches against its epoch) and the epoch block after it

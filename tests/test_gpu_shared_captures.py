@@ -180,3 +180,25 @@ def test_an_eager_append_without_the_sync_of_replays_is_refused():
     bt.check()
     L = bt.append([10, 10])
     bt.check(L)
+
+
+def test_the_first_call_is_not_captured():
+    """It zeroes the cache's state, and a replay would do so again behind later appends."""
+    bt = Shared("affine4", 2, 1, 4, 64, 512, num_pages=4, seed=15)
+    q = torch.randn(2, 4, 1, 64, device="cuda").bfloat16()
+    k = q[:, :1].contiguous()
+    out, ws = torch.zeros_like(q), torch.empty(bt.gc.attend_shared_workspace(), dtype=torch.uint8, device="cuda")
+    calls = (lambda: bt.gc.attend_decode_shared(q, out=out, workspace=ws),
+             lambda: bt.gc.attend_prefill_shared(q, out=out, workspace=ws),
+             lambda: bt.gc.attend_decode(q, out=out), lambda: bt.gc.append_ragged(k, k, [0, 0]))
+    for call in calls:
+        _refused_in_capture(call)
+    bt.append([300, 2])
+    bt.check(300)
+    bt.gc.reset()
+    for call in calls:
+        _refused_in_capture(call)
+    for b in range(2):
+        bt.set(b, bt.hist[b], 0)
+    bt.append([3, 290])
+    bt.check(290)
