@@ -4,6 +4,7 @@
 #include <cstdio>
 #include <cstring>
 #include <algorithm>
+#include <memory>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -19,7 +20,11 @@ thread_local std::string g_last_error;
 kvq_status vfail(kvq_status st, const char* fmt, va_list ap) {
   char buf[512];
   vsnprintf(buf, sizeof buf, fmt, ap);
-  g_last_error = buf;
+  try {
+    g_last_error = buf;
+  } catch (...) {                                        // (no host memory for the words)
+    g_last_error.clear();
+  }
   return st;
 }
 
@@ -308,8 +313,19 @@ kvq_status kvq_create_cache(const kvq_cache_desc* desc, void* dev_buf, size_t by
   if (need == 0) return st;
   if (bytes < need)
     return fail(KVQ_ERR_CAPACITY, "buffer of %zu bytes < %zu needed", bytes, need);
-  kvq_cache* c = new kvq_cache;
-  c->desc = *desc;
+  std::unique_ptr<kvq_cache> c;
+  try {
+    c.reset(new kvq_cache);
+    if (g.layout != KVQ_LAYOUT_UNIFORM) {
+      c->seq_T.assign(g.B, 0);
+      c->seq_n.assign(g.B, 0);
+      c->seq_pages.assign(g.B, std::vector<int>());
+    }
+    c->desc = *desc;
+    if (g.layout == KVQ_LAYOUT_PAGED) pages_reset(c.get());
+  } catch (...) {
+    return fail(KVQ_ERR_CAPACITY, "kvq_create_cache: out of host memory");
+  }
   c->g = g;
   c->base = static_cast<char*>(dev_buf);
   c->bytes = bytes;
@@ -332,12 +348,8 @@ kvq_status kvq_create_cache(const kvq_cache_desc* desc, void* dev_buf, size_t by
       c->g.shared_plan =
           reinterpret_cast<int32_t*>(p + align256((size_t)g.B * g.max_pages * 4));
     }
-    c->seq_T.assign(g.B, 0);
-    c->seq_n.assign(g.B, 0);
-    c->seq_pages.assign(g.B, std::vector<int>());
-    if (g.layout == KVQ_LAYOUT_PAGED) pages_reset(c);
   }
-  *out = c;
+  *out = c.release();
   g_last_error.clear();
   return KVQ_OK;
 }
@@ -448,9 +460,8 @@ kvq_status kvq_append_pack(kvq_cache* cache, const void* k, const void* v, int L
 // Ragged and paged layouts: per-sequence counts on the host and the device,
 // and the page pool's allocator (host side; the device reads the table)
 // ---------------------------------------------------------------------------
-kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v, int L,
-                                  const int* n, void* stream) {
-  if (!cache) return fail(KVQ_ERR_ARG, "cache is NULL");
+static kvq_status append_ragged(kvq_cache* cache, const void* k, const void* v, int L, const int* n,
+                                void* stream) {
   const Geom& g = cache->g;
   if (g.layout == KVQ_LAYOUT_UNIFORM)
     return fail(KVQ_ERR_UNSUPPORTED, "kvq_append_pack_ragged needs a ragged or paged cache");
@@ -480,6 +491,10 @@ kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v
   if (need_pages > cache->n_free)
     return fail(KVQ_ERR_CAPACITY, "the append needs %d pages, %d are free", need_pages,
                 cache->n_free);
+  std::vector<int> room(g.B, g.Tmax);
+  if (need_pages > 0)                                    // (nothing is allocated once pages are taken)
+    for (int b = 0; b < g.B; ++b)
+      cache->seq_pages[b].reserve((cache->seq_T[b] + (int64_t)cnt[b] + kPageTok - 1) / kPageTok);
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
   bool captured = false;
@@ -507,7 +522,6 @@ kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v
       if (e != cudaSuccess) return cuda_fail(e, "kvq_append_pack_ragged page table");
     }
   }
-  std::vector<int> room(g.B, g.Tmax);
   if (g.layout == KVQ_LAYOUT_PAGED)
     for (int b = 0; b < g.B; ++b)
       room[b] = captured ? -1 : (int)std::min<int64_t>(g.Tmax, (int64_t)cache->seq_pages[b].size() * kPageTok);
@@ -521,6 +535,16 @@ kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v
   }
   cache->T = tmax;
   return KVQ_OK;
+}
+
+kvq_status kvq_append_pack_ragged(kvq_cache* cache, const void* k, const void* v, int L,
+                                  const int* n, void* stream) {
+  if (!cache) return fail(KVQ_ERR_ARG, "cache is NULL");
+  try {
+    return append_ragged(cache, k, v, L, n, stream);
+  } catch (...) {                                        // (its lists, before anything is changed)
+    return fail(KVQ_ERR_CAPACITY, "kvq_append_pack_ragged: out of host memory");
+  }
 }
 
 int kvq_seq_tokens(const kvq_cache* cache, int b) {

@@ -1,7 +1,11 @@
 // A CUDA runtime that launches nothing, for the library's host code: a call can be made to
-// fail, and the words that reach the device's plan of shared pages are kept in `plan`.
+// fail, as can an allocation on the host, and the words that reach the device's plan of shared
+// pages are kept in `plan`.
 #include <stdint.h>
+#include <stdlib.h>
 #include <string.h>
+
+#include <new>
 
 namespace {
 struct Kernel {
@@ -12,13 +16,28 @@ Kernel kernels[4096];
 int n_kernels, fail_name_at = -1, launches, last_error;
 char fail_name[64];
 int32_t plan[1 << 14];
+int fail_new = -1;
 }  // namespace
+
+void* operator new(size_t n) {
+  if (fail_new >= 0 && fail_new-- == 0) throw std::bad_alloc();
+  if (void* p = malloc(n ? n : 1)) return p;
+  throw std::bad_alloc();
+}
+void operator delete(void* p) noexcept { free(p); }
+void operator delete(void* p, size_t) noexcept { free(p); }
 
 extern "C" {
 // The next launch but `after` of a kernel whose name holds `part` fails.
 void fake_fail(const char* part, int after) {
   strncpy(fail_name, part, sizeof fail_name - 1);
   fail_name_at = after;
+}
+// The next allocation but `after` fails; returns what was left of that before.
+int fake_no_memory(int after) {
+  const int was = fail_new;
+  fail_new = after;
+  return was;
 }
 int fake_launches() { return launches; }
 int32_t* fake_plan() { return plan; }

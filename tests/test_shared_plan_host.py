@@ -141,3 +141,47 @@ def test_an_attention_call_says_so_when_the_plan_cannot_be_sent(lib):
     assert x.decode() == 0 and lib.fake_launches() == n + 4     # the words, then the three kernels
     assert x.decode() == 0 and lib.fake_launches() == n + 7
     lib.kvq_destroy_cache(x.h)
+
+
+def test_no_host_memory(lib):
+    """Each allocation of each call fails in turn: the call says so (or, where the tree of shared runs
+    alone had no room, goes on without one), nothing is half done, and made again it succeeds."""
+    from paper_2609_04263_gb300 import kvq
+    plans = _plans(lib)
+
+    def pages(h):
+        return (lib.kvq_free_pages(h), [lib.kvq_seq_tokens(h, b) for b in range(B)],
+                [lib.kvq_seq_pages(h, b, None, 0) for b in range(B)])
+    for i, plan in enumerate(plans):
+        for k in range(200):
+            x = Host(lib)
+            for before in _steps(x)[:i]:
+                assert before() == 0
+            was = pages(x.h)
+            lib.fake_no_memory(k)
+            st = _steps(x)[i]()
+            reached = lib.fake_no_memory(-1) < 0
+            assert st in (0, kvq.KVQ_ERR_CAPACITY)
+            if st:
+                assert pages(x.h) == was
+                assert _steps(x)[i]() == 0
+            assert x.decode() == 0
+            if not reached or st or x.plan().any():
+                np.testing.assert_array_equal(x.plan(), plan)
+            lib.kvq_destroy_cache(x.h)
+            if not reached:
+                break
+        else:
+            raise AssertionError("more than 200 allocations")
+    d = kvq.kvq_cache_desc(fmt=kvq.KVQ_FMT_AFFINE, key_bits=4, value_bits=4, group_size=32, batch=B, kv_heads=2,
+                           q_heads=8, head_dim=64, max_tokens=4096, dtype=kvq.KVQ_BF16,
+                           layout=kvq.KVQ_LAYOUT_PAGED, num_pages=60)
+    for k in range(50):
+        h = ctypes.c_void_p()
+        lib.fake_no_memory(k)
+        st = lib.kvq_create_cache(ctypes.byref(d), 1 << 32, lib.kvq_cache_bytes(ctypes.byref(d)), ctypes.byref(h))
+        reached = lib.fake_no_memory(-1) < 0
+        assert (st == kvq.KVQ_ERR_CAPACITY and not h.value) if reached else st == 0
+        if not reached:
+            break
+    assert 3 <= k < 50
