@@ -66,6 +66,9 @@ size_t layout(const kvq_cache_desc* d, Geom* g, size_t off[KVQ_NUM_PLANES],
   if (d->batch <= 0 || d->kv_heads <= 0 || d->q_heads <= 0 || d->max_tokens <= 0) {
     fail(KVQ_ERR_SHAPE, "batch, kv_heads, q_heads and max_tokens must be positive"); return 0;
   }
+  if (d->max_tokens > INT32_MAX - 255) {                 // (rows are padded)
+    fail(KVQ_ERR_SHAPE, "max_tokens %d above 2^31 - 256", d->max_tokens); return 0;
+  }
   if (d->q_heads % d->kv_heads != 0) {
     fail(KVQ_ERR_SHAPE, "q_heads %d is not a multiple of kv_heads %d", d->q_heads, d->kv_heads);
     return 0;
@@ -124,6 +127,14 @@ size_t layout(const kvq_cache_desc* d, Geom* g, size_t off[KVQ_NUM_PLANES],
     }
     if (d->layout == KVQ_LAYOUT_PAGED && d->num_pages <= 0) {
       fail(KVQ_ERR_SHAPE, "a paged cache needs num_pages > 0"); return 0;
+    }
+    // rows of the pool and entries of the page table are counted in 32 bits
+    if (d->layout == KVQ_LAYOUT_PAGED &&
+        (d->num_pages > INT32_MAX / kPageTok ||
+         d->batch * (((int64_t)d->max_tokens + kPageTok - 1) / kPageTok) > INT32_MAX)) {
+      fail(KVQ_ERR_SHAPE, "%d pages, or tables of %d sequences of %d tokens, are more than 2^31 can count",
+           d->num_pages, d->batch, d->max_tokens);
+      return 0;
     }
   }
   const int B = d->batch, H = d->kv_heads, Tm = d->max_tokens;
