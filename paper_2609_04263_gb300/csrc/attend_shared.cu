@@ -1862,8 +1862,8 @@ static kvq_status attend_shared(kvq_cache* cache, const void* q, int L, int n_q_
   if (!q || !out || !workspace) return set_error(KVQ_ERR_ARG, "q, out or workspace is NULL");
   if (reinterpret_cast<uintptr_t>(q) % 16 || reinterpret_cast<uintptr_t>(out) % 16)
     return set_error(KVQ_ERR_ARG, "q and out must be 16-byte aligned");
-  if (!(scale > 0.f) || scale > 3.0e38f)
-    return set_error(KVQ_ERR_ARG, "softmax_scale must be positive and finite");
+  if (!(scale > 0.f) || scale > 2.35e38f)                // (scores in log2 units: times 1.4427)
+    return set_error(KVQ_ERR_ARG, "softmax_scale must be positive and below 2.35e38");
   if (n_q_heads != g.Hq)
     return set_error(KVQ_ERR_SHAPE, "n_q_heads %d != cache q_heads %d", n_q_heads, g.Hq);
   if (!decode)

@@ -1,7 +1,8 @@
-"""Sizes that 32 bits cannot count, refused where a paged cache is made (no GPU)."""
+"""Sizes that 32 bits cannot count, refused where a paged cache is made, and other
+arguments that no kernel could work with (no GPU)."""
 import pytest
 
-from tests.test_pages_abi import _cache, _refused, kvq  # noqa: F401  (a fixture)
+from tests.test_pages_abi import P, _cache, _refused, kvq, paged  # noqa: F401  (fixtures)
 
 
 @pytest.mark.parametrize("kw", [dict(num_pages=1 << 23), dict(num_pages=2 ** 31 - 1),
@@ -21,3 +22,10 @@ def test_the_largest_that_can_be_counted(kvq, kw, gib):  # noqa: F811
     d.update(kw)
     n = kvq.kvq_cache_bytes(kvq.kvq_cache_desc(**d)) / 2 ** 30
     assert gib * 0.999 < n < gib * 1.1
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 3.0e38, 3.4e38])
+def test_scales_that_overflow_in_log2_units(kvq, paged, scale):  # noqa: F811
+    n = kvq.kvq_attend_shared_workspace(paged, 1)
+    _refused(kvq, kvq.KVQ_ERR_ARG, kvq.kvq_attend_decode_shared, paged, P, 8, scale, P, P, n)
+    _refused(kvq, kvq.KVQ_ERR_ARG, kvq.kvq_attend_prefill_shared, paged, P, 1, 8, scale, P, P, n)
