@@ -136,6 +136,8 @@ class Cache:
     def append_ragged(self, k, v, n=None) -> None:
         """Ragged / paged caches: sequence b appends the first n[b] of its
         rows of k, v [B, H, L, D] (all L when n is None)."""
+        if n is not None and len(n) != self.desc.batch:
+            raise ValueError(f"{len(n)} counts for {self.desc.batch} sequences")
         kvq.kvq_append_pack_ragged(self.handle, _ptr(k), _ptr(v), k.shape[2], n, _stream())
 
     def seq_tokens(self, b) -> int:

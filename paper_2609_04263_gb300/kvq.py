@@ -315,27 +315,28 @@ def kvq_seq_pages(handle, b) -> list:
     return [buf[i] for i in range(n)]
 
 
-
-def _ints(x):
-    """A host array of C ints (the caller keeps it while the call reads it), and its address."""
+def _ints(x, n):
+    """A host array of n C ints (the caller keeps it while the call reads it), and its address."""
     if x is None:
         return None, None
     a = array("i", x)
+    if len(a) != n:
+        raise ValueError(f"lists of different lengths: {len(a)} and {n}")
     return a, a.buffer_info()[0]
 
 
 def kvq_seq_fork(handle, src, dst, tokens=None, stream=0) -> None:
-    (a, pa), (b, pb), (c, pc) = _ints(src), _ints(dst), _ints(tokens)
+    (a, pa), (b, pb), (c, pc) = (_ints(x, len(dst)) for x in (src, dst, tokens))
     _check(lib().kvq_seq_fork(handle, len(dst), pa, pb, pc, stream or None))
 
 
 def kvq_seq_copy(to, source, src, dst, tokens=None, stream=0) -> None:
-    (a, pa), (b, pb), (c, pc) = _ints(src), _ints(dst), _ints(tokens)
+    (a, pa), (b, pb), (c, pc) = (_ints(x, len(dst)) for x in (src, dst, tokens))
     _check(lib().kvq_seq_copy(to, source, len(dst), pa, pb, pc, stream or None))
 
 
 def kvq_seq_truncate(handle, seqs, tokens, stream=0) -> None:
-    (a, pa), (b, pb) = _ints(seqs), _ints(tokens)
+    (a, pa), (b, pb) = (_ints(x, len(seqs)) for x in (seqs, tokens))
     _check(lib().kvq_seq_truncate(handle, len(seqs), pa, pb, stream or None))
 
 

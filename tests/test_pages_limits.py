@@ -29,3 +29,22 @@ def test_scales_that_overflow_in_log2_units(kvq, paged, scale):  # noqa: F811
     n = kvq.kvq_attend_shared_workspace(paged, 1)
     _refused(kvq, kvq.KVQ_ERR_ARG, kvq.kvq_attend_decode_shared, paged, P, 8, scale, P, P, n)
     _refused(kvq, kvq.KVQ_ERR_ARG, kvq.kvq_attend_prefill_shared, paged, P, 1, 8, scale, P, P, n)
+
+
+def test_lists_that_the_call_would_read_past(kvq, paged):  # noqa: F811
+    """The binding gives one count: that of the other lists is checked."""
+    for call, args in ((kvq.kvq_seq_fork, ([0], [1, 2])), (kvq.kvq_seq_fork, ([0, 0], [1, 2], [0])),
+                       (kvq.kvq_seq_copy, (paged, [0], [1, 2])), (kvq.kvq_seq_copy, (paged, [0, 0], [1, 2], [0])),
+                       (kvq.kvq_seq_truncate, ([0, 1], [0])), (kvq.kvq_seq_truncate, ([], [0]))):
+        with pytest.raises(ValueError):
+            call(paged, *args)
+
+
+def test_an_append_needs_a_count_a_sequence(kvq):  # noqa: F811
+    import types
+
+    from paper_2609_04263_gb300 import api
+    cache = types.SimpleNamespace(desc=types.SimpleNamespace(batch=4), handle=None)
+    for n in ([], [1], [1] * 5):
+        with pytest.raises(ValueError):
+            api.Cache.append_ragged(cache, None, None, n)
