@@ -1376,7 +1376,8 @@ leaf_kernel(Geom g, const __nv_bfloat16* __restrict__ q, float scale, LeafSched*
       for (int mt = 0; mt < 2; ++mt) {
         S[mt][0] = S[mt][1] = S[mt][2] = S[mt][3] = 0.f;
         const int ta = t0 + 16 * mt + gid, tb = ta + 8;
-        const __nv_bfloat16 *ka = kw + slot_of(16 * mt + gid) * D, *kb = kw + slot_of(16 * mt + gid + 8) * D;
+        const __nv_bfloat16 *ka = kw + (int64_t)slot_of(16 * mt + gid) * D,
+                            *kb = kw + (int64_t)slot_of(16 * mt + gid + 8) * D;
         const uint4 z = make_uint4(0, 0, 0, 0);
         uint4 va[D / 32], vb[D / 32];                  // all under way before the first is used
 #pragma unroll
@@ -1499,7 +1500,7 @@ leaf_kernel(Geom g, const __nv_bfloat16* __restrict__ q, float scale, LeafSched*
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int j = 16 * mt + 8 * (i >> 1) + 2 * tid + (i & 1);
-          const __nv_bfloat16* vr = vw + slot_of(j) * D;
+          const __nv_bfloat16* vr = vw + (int64_t)slot_of(j) * D;
 #pragma unroll
           for (int c = 0; c < CH / 8; ++c)
             wv[c][i] = j < nv ? reinterpret_cast<const uint4*>(vr)[c] : make_uint4(0, 0, 0, 0);

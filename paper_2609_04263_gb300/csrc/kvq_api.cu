@@ -94,8 +94,8 @@ size_t layout(const kvq_cache_desc* d, Geom* g, size_t off[KVQ_NUM_PLANES],
       return 0;
     }
   }
-  if (d->fmt == KVQ_FMT_KIVI && d->residual_tokens < 0) {
-    fail(KVQ_ERR_SHAPE, "residual_tokens must be >= 0"); return 0;
+  if (d->fmt == KVQ_FMT_KIVI && (d->residual_tokens < 0 || d->residual_tokens > INT32_MAX - 128)) {
+    fail(KVQ_ERR_SHAPE, "residual_tokens must be >= 0 and below 2^31 - 128"); return 0;
   }
   if (d->fmt == KVQ_FMT_KVARN) {
     if (d->sink_tokens < 0 || d->norm_iters < 0 || d->norm_iters > 64) {

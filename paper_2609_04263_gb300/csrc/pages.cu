@@ -209,7 +209,8 @@ take_kernel(const __grid_constant__ Geom to, const __grid_constant__ Geom from, 
     const int slot0 = lo % to.ring, n0 = min(n, to.ring - slot0);
     char* d = reinterpret_cast<char*>(plane_ptr<__nv_bfloat16>(to, which, t.dst, h, 0, 0));
     const char* s = reinterpret_cast<const char*>(plane_ptr<__nv_bfloat16>(from, which, t.src, h, 0, 0));
-    copy16(s + slot0 * row, d + slot0 * row, n0 * row / 16, threadIdx.x, kThreads);
+    const int64_t at = (int64_t)slot0 * row;
+    copy16(s + at, d + at, n0 * row / 16, threadIdx.x, kThreads);
     copy16(s, d, (n - n0) * row / 16, threadIdx.x, kThreads);
     return;
   }
