@@ -205,7 +205,7 @@ __device__ void split_issue(const Geom& g, int b, int hkv, const SplitPlan& sp, 
   uint32_t total = 2 * code_bytes + kmeta + vmeta;
   if (zero_planes) total += kmeta + vmeta;
   mbar_expect_tx(&bars[stage], total);
-  // a chunk is one 64-token page of a paged cache: tok_ptr finds its rows
+  // a chunk lies in one page of a paged cache: tok_ptr finds its rows
   bulk_g2s(st + C::KC_OFF, tok_ptr<uint8_t>(g, KVQ_PLANE_K_CODES, b, hkv, c0), code_bytes,
            &bars[stage]);
   bulk_g2s(st + C::VC_OFF, tok_ptr<uint8_t>(g, KVQ_PLANE_V_CODES, b, hkv, c0), code_bytes,

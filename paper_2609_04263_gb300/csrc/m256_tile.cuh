@@ -122,7 +122,7 @@ __device__ __forceinline__ void load_raw(const Geom& g, int b, int h, int t0, un
   using S = M256Layout<D, BITS>;
   constexpr uint32_t CB = kTok * S::CROW;
   mbar_expect_tx(bar, raw_bytes<D, BITS, FMT>());
-  // a tile is one 64-token page of a paged cache: tok_ptr finds its rows
+  // a tile lies in one page of a paged cache: tok_ptr finds its rows
   bulk_copy(raw + S::RKC, tok_ptr<uint8_t>(g, KVQ_PLANE_K_CODES, b, h, t0), CB, bar);
   bulk_copy(raw + S::RVC, tok_ptr<uint8_t>(g, KVQ_PLANE_V_CODES, b, h, t0), CB, bar);
   // KIVI: two key blocks of D channels
@@ -159,16 +159,16 @@ __device__ __forceinline__ void split_store(const uint64_t (&k2)[4], unsigned ch
   *reinterpret_cast<uint4*>(lo_dst) = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-// Producers (build_keys, build_values; build_tile: both): reconstruct this CTA's share of the
-// K and V operand tiles of KV tile t0 from the packed tile in `raw` (tokens below tq), the KIVI residual ring
-// (tq <= t < T) or zeros (t >= T).  tid 0..127:
+// Producers: reconstruct this CTA's share of the K and V operand tiles of KV tile t0 from the
+// packed tile in `raw` (tokens below tq), the KIVI residual ring (tq <= t < T) or zeros
+// (t >= T).  tid 0..127:
 //   K: thread (tk = tid % KT, hf = tid / KT): token KT rank + tk, channels
 //      KC hf .. KC hf + KC - 1.
 //   V: thread (tb = tid % 8, vq = tid % NP / 8): tokens 8 tb .. 8 tb + 7 and
 //      channels CV vq .. CV vq + CV - 1 of this CTA's, in half2 arithmetic, stored
 //      as rows of the transposed tile (half a 16-byte chunk per row and trip).
 template <int D, int BITS, int FMT>
-__device__ __forceinline__ void build_keys(const Geom& g, int b, int h, int t0, int T, int tq,
+__device__ __forceinline__ void build_tile(const Geom& g, int b, int h, int t0, int T, int tq,
                                            int tid, int rank, const unsigned char* raw, float* ksz,
                                            unsigned char* kv) {
   using S = M256Layout<D, BITS>;
@@ -267,15 +267,6 @@ __device__ __forceinline__ void build_keys(const Geom& g, int b, int h, int t0, 
       *reinterpret_cast<uint4*>(base + S::KL + sw128(tk, cc & 7)) = make_uint4(0, 0, 0, 0);
     }
   }
-}
-
-template <int D, int BITS, int FMT>
-__device__ __forceinline__ void build_values(const Geom& g, int b, int h, int t0, int T, int tq,
-                                             int tid, int rank, const unsigned char* raw,
-                                             unsigned char* kv) {
-  using S = M256Layout<D, BITS>;
-  constexpr bool KIVI = FMT == KVQ_FMT_KIVI;
-  constexpr bool SYM = FMT == KVQ_FMT_SYMMETRIC;
   constexpr int CV = S::CV;
   // V^T tile: rows CV vq + e, 16-byte chunk tb (tokens 8 tb ..)
   const int tb = tid & 7, vq = tid % S::NP >> 3;
@@ -348,14 +339,6 @@ __device__ __forceinline__ void build_values(const Geom& g, int b, int h, int t0
   for (int e = 0; e < CV; ++e)
     *reinterpret_cast<uint2*>(kv + S::VT + sw128(CV * vq + e, tb) + 4 * p0) = make_uint2(out[e][0], out[e][1]);
   }
-}
-
-template <int D, int BITS, int FMT>
-__device__ __forceinline__ void build_tile(const Geom& g, int b, int h, int t0, int T, int tq,
-                                           int tid, int rank, const unsigned char* raw, float* ksz,
-                                           unsigned char* kv) {
-  build_keys<D, BITS, FMT>(g, b, h, t0, T, tq, tid, rank, raw, ksz, kv);
-  build_values<D, BITS, FMT>(g, b, h, t0, T, tq, tid, rank, raw, kv);
 }
 
 }  // namespace m256
