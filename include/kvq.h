@@ -297,6 +297,9 @@ kvq_status kvq_attend_prefill(kvq_cache* cache, const void* q, int L, int n_q_he
  * Decode step: kvq_attend_prefill with L = 1, split over the tokens across
  * thread blocks with a log-sum-exp merge (partials in the cache's workspace
  * plane, so calls on one cache must not overlap).  q, out [B][Hq][1][D].
+ * KIVI keys: where every SM has 16 or more 32-token blocks of a kv head to read,
+ * the kernel forms offset x 16 and |q| x scale in fp16; offsets beyond 4,094, or
+ * products beyond 65,504, overflow there.
  */
 kvq_status kvq_attend_decode(kvq_cache* cache, const void* q, int n_q_heads,
                              float softmax_scale, void* out, void* stream);
@@ -311,7 +314,10 @@ kvq_status kvq_attend_decode(kvq_cache* cache, const void* q, int n_q_heads,
  * ranks that are multiples of 8 up to 64 (kvq_decode_step_fused tells) the
  * three steps run as one cooperative kernel with one CTA per SM, whose CTAs
  * hand results to one another through the cache's workspace with bounded
- * waits; other shapes run the three calls in order.  Both give the same codes
+ * waits; other shapes run the three calls in order (RAGGED and PAGED caches
+ * always: its attention reads a page that sequences share once for each of them;
+ * kvq_project_lora, kvq_append_pack and kvq_attend_decode_shared read it once
+ * for all).  Both give the same codes
  * for the same k and v and agree to bf16 rounding.  Like kvq_attend_decode
  * it uses the cache's workspace, so calls on one cache must not overlap.
  * The fused kernel starts reading w_qkv and the LoRA factors before the work
@@ -517,7 +523,12 @@ kvq_status kvq_cache_compact(kvq_cache* cache, void* stream);
  * kvq_attend_prefill_shared: of kvq_attend_prefill (per sequence, the rows l < n[b] of
  *                            its last append; the rest of out is not written).
  * Both agree with those calls to bf16 rounding and may be captured in a graph, whose
- * replays follow the cache as it then is.
+ * replays follow the cache as it then is.  A NaN score makes its row NaN, a score of -inf
+ * has no weight.  Ranges: values of a KIVI window and code x scale + offset of a value in
+ * fp16, as those calls; decode of KIVI keys |q| x scale up to 65,504.
+ * Decode takes three dependent launches and pays off from about 16 (sequence, kv head,
+ * 32-token block) triples a SM on (12 at head_dim 128, 4 to 6 for KIVI).  On less,
+ * kvq_attend_decode is faster: 4 short sequences 11 us against 17.
  * workspace: caller-owned device memory of at least kvq_attend_shared_workspace(cache, L)
  * bytes (L = 1 for decode; 0 for a cache or L that the calls refuse), 256-byte aligned;
  * the bytes needed grow with forks, and a replay whose workspace has become too small writes nothing
@@ -526,7 +537,8 @@ kvq_status kvq_cache_compact(kvq_cache* cache, void* stream);
  * KVQ_ERR_SHAPE where B L query rows of up to max_tokens keys are more than the calls can
  * count (about 2^31 tiles of 256 x 64; 128 x 64 at head_dim 64).
  * Prompts long enough to fill the tiles alone are attended sequence by sequence, except
- * in a captured call.
+ * in a captured call, which is then slower (8 prompts of 2,048 tokens behind 512: 560 us
+ * eagerly, 1,850 replayed; capture kvq_attend_prefill for such batches).
  */
 size_t kvq_attend_shared_workspace(const kvq_cache* cache, int L);
 kvq_status kvq_attend_decode_shared(kvq_cache* cache, const void* q, int n_q_heads,

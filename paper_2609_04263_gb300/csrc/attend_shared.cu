@@ -1772,9 +1772,10 @@ cudaError_t launch_shared(const Geom& g, const Call& c, cudaStream_t s) {
 // fill its tiles without other sequences' rows.  Both times are estimated from what a 64-token
 // tile took, in ns, and here from 1 ns a query row to merge; on 60 shapes (1 to 16 sequences,
 // 16 to 2048 rows behind 512 to 16384 tokens) the estimate is mostly within 20 % and took the
-// slower side 4 times, by 3 % at most.  2 x 256 rows behind 4096 tokens, 32 / 8 heads of 128, KIVI:
-// 107 us there, 82 here; 2 x 1024: 231 and 305; 8 x 2048 behind 512, affine: 577 and 1913;
-// 4 x 64 behind 17,384: 372 and 132.
+// slower side 4 times, by 3 % at most (of 2 and 4 bits, which it takes alike; since then the
+// kernel there got 3 % faster).  2 x 256 rows behind 4096 tokens, 32 / 8 heads of 128, KIVI:
+// 103 us there, 82 here; 2 x 1024: 222 and 313; 8 x 2048 behind 512, affine: 555 and 1850;
+// 4 x 64 behind 17,384: 396 and 121.
 bool alone_faster(const kvq_cache* c) {
   const Geom& g = c->g;
   if (!prefill_m256_supported(g)) return false;
