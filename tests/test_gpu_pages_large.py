@@ -1,5 +1,7 @@
 """KIVI windows whose slots lie more than 2^31 bytes and elements from their start: forks of them, and
 decode attention over them."""
+import gc
+
 import pytest
 import torch
 
@@ -12,6 +14,13 @@ pytestmark = pytest.mark.gpu
 @pytest.fixture(scope="module", autouse=True)
 def _gpu():
     require_gpu()
+
+
+@pytest.fixture(autouse=True)
+def _no_graph_left():
+    """Graphs that caught exceptions' frames still hold are freed here: freed in the middle of another
+    capture, they would end that one."""
+    gc.collect()
 
 
 def test_a_window_of_more_than_2_to_the_24_tokens():

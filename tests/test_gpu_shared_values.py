@@ -192,3 +192,46 @@ def test_large_offsets(fmt, D):
             _check(bt, _decodes(bt, q.cuda()), q)
         else:
             _check(bt, _prefills(bt, q.cuda(), L), q, bt.n_last)
+
+
+@pytest.mark.parametrize("fmt,H,Hq,D", [("affine4", 1, 1, 64), ("sym2", 1, 16, 128), ("kivi2", 3, 3, 64),
+                                        ("kivi4", 1, 5, 128)])
+def test_the_smallest_caches(fmt, H, Hq, D):
+    """One sequence (which nothing can be forked into), one token, one page, one row."""
+    bt = Edited(fmt, 1, H, Hq, D, 256, num_pages=1, seed=1)
+    q = _queries(bt, 1, 2)
+    assert all(torch.all(x == 0) for x in _decodes(bt, q.cuda()).values())
+    for n in (1, 1, 31, 200, 23):
+        L = bt.append([n])
+        _check(bt, _decodes(bt, q.cuda()), q)
+        p = _queries(bt, L, 3)
+        _check(bt, _prefills(bt, p.cuda(), L), p)
+
+
+def test_a_workspace_of_two_captured_calls():
+    """Two caches' graphs over one workspace, replayed in turn on one stream: a call leaves nothing
+    in it that a later one reads."""
+    a = Edited("kivi2", 6, 2, 8, 128, 1200, num_pages=30, seed=5)
+    b = Edited("affine4", 9, 1, 4, 64, 1200, num_pages=40, seed=6)
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for bt in (a, b):
+        bt.append([700] + [0] * (bt.B - 1))
+        bt.fork([0] * (bt.B - 1), list(range(1, bt.B)))
+        L = bt.append([1 + i for i in range(bt.B)])
+        q, p = _queries(bt, 1, 7), _queries(bt, L, 8)
+        qd, pd = q.cuda(), p.cuda()
+        for call, x, host, rows in ((bt.gc.attend_decode_shared, qd, q, None), (bt.gc.attend_prefill_shared, pd, p, bt.n_last)):
+            out = torch.zeros_like(x)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                call(x, out=out, workspace=ws)
+            graphs.append((bt, g, out, host, rows, x))
+    for order in ((0, 1, 2, 3), (3, 1, 2, 0), (2, 0, 3, 1)):
+        for i in order:
+            graphs[i][2].zero_()
+            graphs[i][1].replay()
+        torch.cuda.synchronize()
+        for bt, _, out, host, rows, _ in graphs:
+            _check(bt, {"replayed": out}, host, rows)
