@@ -473,7 +473,8 @@ int kvq_seq_pages(const kvq_cache* cache, int b, int* pages, int max_pages);
  * append, kvq_cache_sync comes first, and the calls cannot be captured themselves
  * (KVQ_ERR_UNSUPPORTED).  New pages are the pool's lowest-numbered free ones, taken in
  * the order of the entries and of their tokens.  After KVQ_ERR_CUDA (a launch failed) the
- * sequences named hold nothing defined until they are released or the cache is reset.
+ * sequences that the call changes (kvq_cache_compact: all) hold nothing defined until they
+ * are released or the cache is reset.
  *
  * A sequence whose last tokens are given up starts its next append there; the rows
  * behind its count are left as they were.  Its count of newly appended tokens (the rows

@@ -502,7 +502,16 @@ static kvq_status append_ragged(kvq_cache* cache, const void* k, const void* v, 
   if (need_pages > cache->n_free)
     return fail(KVQ_ERR_CAPACITY, "the append needs %d pages, %d are free", need_pages,
                 cache->n_free);
-  std::vector<int> room(g.B, g.Tmax);
+  std::vector<int> room(g.B, g.Tmax), held(g.B, 0);
+  for (int b = 0; b < g.B; ++b) held[b] = (int)cache->seq_pages[b].size();
+  // (a call that fails on the way gives its pages back: the table may not have their entries)
+  const auto failed = [&](cudaError_t e, const char* where) {
+    for (int b = 0; b < g.B; ++b)
+      for (; (int)cache->seq_pages[b].size() > held[b]; cache->seq_pages[b].pop_back())
+        page_drop(cache, cache->seq_pages[b].back());
+    (void)cudaGetLastError();                            // (reported here, not by the next call)
+    return cuda_fail(e, where);
+  };
   if (need_pages > 0)                                    // (nothing is allocated once pages are taken)
     for (int b = 0; b < g.B; ++b)
       cache->seq_pages[b].reserve((cache->seq_T[b] + (int64_t)cnt[b] + kPageTok - 1) / kPageTok);
@@ -530,14 +539,14 @@ static kvq_status append_ragged(kvq_cache* cache, const void* k, const void* v, 
       // before the call returns, so pg may change afterwards)
       e = cudaMemcpyAsync(g.page_table + (size_t)b * g.max_pages + have, pg.data() + have,
                           (size_t)(want - have) * sizeof(int32_t), cudaMemcpyHostToDevice, s);
-      if (e != cudaSuccess) return cuda_fail(e, "kvq_append_pack_ragged page table");
+      if (e != cudaSuccess) return failed(e, "kvq_append_pack_ragged page table");
     }
   }
   if (g.layout == KVQ_LAYOUT_PAGED)
     for (int b = 0; b < g.B; ++b)
       room[b] = captured ? -1 : (int)std::min<int64_t>(g.Tmax, (int64_t)cache->seq_pages[b].size() * kPageTok);
   e = launch_append_ragged(g, L, k, v, cnt.data(), room.data(), s);
-  if (e != cudaSuccess) return cuda_fail(e, "kvq_append_pack_ragged launch");
+  if (e != cudaSuccess) return failed(e, "kvq_append_pack_ragged launch");
   int tmax = 0;
   for (int b = 0; b < g.B; ++b) {
     cache->seq_T[b] += cnt[b];

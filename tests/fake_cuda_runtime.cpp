@@ -68,7 +68,10 @@ int cudaMemsetAsync(void*, int, size_t n, void*) {
   if (n >= 2048) memset(plan, 0, sizeof plan);           // the cache's state
   return 0;
 }
-int cudaMemcpyAsync() { return 0; }
+int cudaMemcpyAsync() {
+  if (fail_name_at >= 0 && !strcmp(fail_name, "copy") && fail_name_at-- == 0) return last_error = 1;
+  return 0;
+}
 int cudaDeviceGetAttribute(int* v, int, int) { *v = 152; return 0; }
 int cudaGetDevice(int* d) { *d = 0; return 0; }
 int cudaStreamIsCapturing(void*, int* st) { *st = 0; return 0; }

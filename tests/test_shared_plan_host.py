@@ -185,3 +185,28 @@ def test_no_host_memory(lib):
         if not reached:
             break
     assert 3 <= k < 50
+
+
+@pytest.mark.parametrize("part", [b"copy", b"seq_counts", b"pack_pertoken", b"seq_advance"])
+@pytest.mark.parametrize("after", [0, 1])
+def test_a_failed_append_gives_its_pages_back(lib, part, after):
+    """Pages whose entries may not have reached the table are no sequence's; the next append takes
+    them anew and sends their entries."""
+    from paper_2609_04263_gb300 import kvq
+    x = Host(lib)
+    assert x.append([300, 0, 10, 0, 0]) == 0
+
+    def pages():
+        return (lib.kvq_free_pages(x.h), [lib.kvq_seq_pages(x.h, b, None, 0) for b in range(B)],
+                [lib.kvq_seq_tokens(x.h, b) for b in range(B)])
+    was = pages()
+    lib.fake_fail(part, after)
+    st = x.append([300, 600, 0, 1, 0])
+    lib.fake_fail(b"", -1)
+    if st == 0:                               # (the kernel is launched once)
+        assert after == 1 and part != b"copy"
+    else:
+        assert st == kvq.KVQ_ERR_CUDA and pages() == was
+        assert x.append([300, 600, 0, 1, 0]) == 0
+    assert pages() == (60 - 8, [3, 3, 1, 1, 0], [600, 600, 10, 1, 0])
+    lib.kvq_destroy_cache(x.h)
